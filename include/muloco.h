@@ -368,7 +368,7 @@ typedef struct {
   const void* q_gain;              /* [head_dim] of gain_dtype                              */
   const void* k_gain;
   int gain_dtype;                  /* mlc_dtype                                             */
-  const float* cos;                /* [table_rows][rot_dim / 2]; not read if rot_dim is 0   */
+  const float* cos;                /* [table_rows][rot_dim / 2]; not read if either is 0     */
   const float* sin;
   int64_t table_rows;
   const void* positions;           /* [tokens] int64_t or, with positions_32bit, int32_t    */

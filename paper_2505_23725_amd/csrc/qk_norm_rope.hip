@@ -148,7 +148,8 @@ struct Place {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { a[i] += offset; b[i] += offset; }
   }
-  // cos and sin of the lane's pairs (1 and 0 where they pass); a position outside the tables gives NaN
+  // cos and sin of the lane's pairs (1 and 0 where they pass); a position outside the tables reads nothing of them (they may have
+  // no rows at all) and gives NaN
   __device__ __forceinline__ void angles(const QkArgs& g, long token, float (&c)[4], float (&s)[4]) const {
     const long p = g.pos64 ? ((const long*)g.positions)[token] : (long)((const int*)g.positions)[token];
     const bool in = p >= 0 && p < g.table_rows;
@@ -156,12 +157,12 @@ struct Place {
     if constexpr (VEC) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) { c[i] = 1.f; s[i] = 0.f; }
-      if (turned(0)) { Vec4<float>::load(g.cos + at + pair(0), c); Vec4<float>::load(g.sin + at + pair(0), s); }
+      if (in && turned(0)) { Vec4<float>::load(g.cos + at + pair(0), c); Vec4<float>::load(g.sin + at + pair(0), s); }
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        c[i] = turned(i) ? g.cos[at + pair(i)] : 1.f;
-        s[i] = turned(i) ? g.sin[at + pair(i)] : 0.f;
+        c[i] = in && turned(i) ? g.cos[at + pair(i)] : 1.f;
+        s[i] = in && turned(i) ? g.sin[at + pair(i)] : 0.f;
       }
     }
     if (!in)

@@ -190,3 +190,18 @@ def test_refusals():
         mlc.muloco_qk_norm_rope_backward(dq, dk, q, k, wq, wk, cos, sin, pos, torch.empty_like(q), torch.empty_like(k),
                                          torch.empty(64, device=DEV), torch.empty(64, device=DEV), ws)
     assert not qo.any() and not ko.any()
+
+
+@pytest.mark.parametrize("dim,rot", [(64, 64), (20, 12)])
+def test_tables_without_rows_are_not_read(dim, rot):
+    """No position lies in tables of no rows (whose address is NULL): every output and gradient is NaN, as for any other position
+    outside."""
+    q, k, dq, dk, wq, wk, cos, sin, pos = [x.to(DEV) for x in _case(5, 3, 2, dim, rot, torch.bfloat16)]
+    cos, sin = cos[:0].contiguous(), sin[:0].contiguous()
+    assert cos.data_ptr() == 0 and cos.shape == (0, rot // 2)
+    out = [torch.zeros_like(x) for x in (q, k, q, k)]
+    gains = [torch.zeros(dim, device=DEV) for _ in range(2)]
+    ws = torch.empty(mlc.muloco_qk_norm_rope_workspace_bytes(dim), dtype=torch.uint8, device=DEV)
+    mlc.muloco_qk_norm_rope(q, k, wq, wk, cos, sin, pos, *out[:2])
+    mlc.muloco_qk_norm_rope_backward(dq, dk, q, k, wq, wk, cos, sin, pos, *out[2:], *gains, ws)
+    assert all(torch.isnan(x).all() for x in out + gains)

@@ -153,3 +153,11 @@ def test_structures_match_the_header(tmp_path):
             assert C.sizeof(STRUCTS[w[0]]) == int(w[2]), line
         else:
             assert getattr(STRUCTS[w[0]], w[1]).offset == int(w[2]), line
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_tables_without_rows_may_be_null(back):
+    """(refused for what comes behind the tables: an odd address of a bf16 tensor)"""
+    heads = dict(heads={"dq_out" if back else "q": [P + 1, 192, 64]})
+    assert _qk(back, change=dict(table_rows=0, cos=None, sin=None), **heads) == ARG
+    assert _qk(back, change=dict(cos=None, sin=None), **heads) == NULL
