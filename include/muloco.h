@@ -371,7 +371,7 @@ typedef struct {
   const float* cos;                /* [table_rows][rot_dim / 2]; not read if either is 0     */
   const float* sin;
   int64_t table_rows;
-  const void* positions;           /* [tokens] int64_t or, with positions_32bit, int32_t    */
+  const void* positions;           /* [tokens] int64_t or, with positions_32bit, int32_t; not read if rot_dim is 0 */
   int positions_32bit;
   float eps, gain_offset;
   int interleaved;

@@ -1015,7 +1015,7 @@ static int check_qk(const mlc_qk_norm_rope* p) {
       (p->positions_32bit != 0 && p->positions_32bit != 1))
     return MLC_ERR_ARG;
   if (!p->q_gain || (p->k_heads && !p->k_gain)) return MLC_ERR_NULL;
-  if (p->tokens && (!p->positions || (p->rot_dim && p->table_rows && (!p->cos || !p->sin)))) return MLC_ERR_NULL;
+  if (p->tokens && p->rot_dim && (!p->positions || (p->table_rows && (!p->cos || !p->sin)))) return MLC_ERR_NULL;
   const size_t ge = elem_size(p->gain_dtype);
   if ((uintptr_t)p->q_gain % ge || (uintptr_t)p->k_gain % ge || (uintptr_t)p->cos % 4 || (uintptr_t)p->sin % 4 ||
       (uintptr_t)p->positions % (p->positions_32bit ? 4 : 8))

@@ -151,6 +151,11 @@ struct Place {
   // cos and sin of the lane's pairs (1 and 0 where they pass); a position outside the tables reads nothing of them (they may have
   // no rows at all) and gives NaN
   __device__ __forceinline__ void angles(const QkArgs& g, long token, float (&c)[4], float (&s)[4]) const {
+    if (rot == 0) {                                 // the norm alone: no positions
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { c[i] = 1.f; s[i] = 0.f; }
+      return;
+    }
     const long p = g.pos64 ? ((const long*)g.positions)[token] : (long)((const int*)g.positions)[token];
     const bool in = p >= 0 && p < g.table_rows;
     const long at = in ? p * (rot / 2) : 0;

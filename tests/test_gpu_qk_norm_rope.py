@@ -205,3 +205,24 @@ def test_tables_without_rows_are_not_read(dim, rot):
     mlc.muloco_qk_norm_rope(q, k, wq, wk, cos, sin, pos, *out[:2])
     mlc.muloco_qk_norm_rope_backward(dq, dk, q, k, wq, wk, cos, sin, pos, *out[2:], *gains, ws)
     assert all(torch.isnan(x).all() for x in out + gains)
+
+
+@pytest.mark.parametrize("dim,rows", [(64, 0), (20, 0), (64, 3)])
+def test_the_norm_alone_needs_no_positions(dim, rows):
+    """Nothing to turn: whatever the tables' rows and the positions are, the results are those of rotation by nothing."""
+    q, k, dq, dk, wq, wk, _, _, pos = [x.to(DEV) for x in _case(5, 3, 2, dim, 0, torch.float32)]
+    ws = torch.empty(mlc.muloco_qk_norm_rope_workspace_bytes(dim), dtype=torch.uint8, device=DEV)
+
+    def both(empty, positions):
+        out = [torch.zeros_like(x) for x in (q, k, q, k)] + [torch.zeros(dim, device=DEV) for _ in range(2)]
+        mlc.muloco_qk_norm_rope(q, k, wq, wk, empty, empty, positions, *out[:2])
+        mlc.muloco_qk_norm_rope_backward(dq, dk, q, k, wq, wk, empty, empty, positions, *out[2:], ws)
+        return out
+    got = both(torch.empty(rows, 0, device=DEV), pos + 100)
+    args = (to_f64(wq), 0.0, np.zeros((50, 0)), np.zeros((50, 0)), pos.tolist(), 1e-6, False)
+    assert_fp32_close(got[0].cpu(), oracle.forward(to_f64(q), *args), "q")
+    rx, rw = oracle.backward(to_f64(dq), to_f64(q), *args)
+    assert_fp32_close(got[2].cpu(), rx, "dq")
+    assert_fp32_close(got[4].cpu(), rw, "gradient of the gain of q")
+    inside = both(torch.empty(50, 0, device=DEV), pos)
+    assert all(torch.equal(a, b) for a, b in zip(got, inside))

@@ -161,3 +161,10 @@ def test_tables_without_rows_may_be_null(back):
     heads = dict(heads={"dq_out" if back else "q": [P + 1, 192, 64]})
     assert _qk(back, change=dict(table_rows=0, cos=None, sin=None), **heads) == ARG
     assert _qk(back, change=dict(cos=None, sin=None), **heads) == NULL
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_positions_are_not_needed_where_nothing_is_turned(back):
+    heads = dict(heads={"dq_out" if back else "q": [P + 1, 192, 64]})
+    assert _qk(back, change=dict(rot_dim=0, positions=None, cos=None, sin=None), **heads) == ARG
+    assert _qk(back, change=dict(positions=None), **heads) == NULL
