@@ -174,6 +174,12 @@ struct Place {
 #pragma unroll
       for (int i = 0; i < 4; ++i) c[i] = s[i] = __uint_as_float(0x7fc00000u);
   }
+  // pair i turned by that angle; two elements that are passed on have nothing to do with each other (0 times one that is not finite
+  // would be NaN in the other)
+  __device__ __forceinline__ void turn(int i, float a, float b, float c, float s, float& ya, float& yb) const {
+    ya = a * c - (turned(i) ? b * s : 0.f);
+    yb = b * c + (turned(i) ? a * s : 0.f);
+  }
 };
 
 // A workgroup's share: HEADS neighbouring heads, of the queries or of the keys, of every step-th token.  Workgroups with the
@@ -226,8 +232,7 @@ __global__ __launch_bounds__(THREADS) void qk_norm_rope_kernel(QkArgs g) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float na = a[i] * r * wa[i], nb = b[i] * r * wb[i];
-        a[i] = na * c[i] - nb * s[i];
-        b[i] = nb * c[i] + na * s[i];
+        at.turn(i, na, nb, c[i], s[i], a[i], b[i]);
       }
       at.store(out + h * out_step, a, b);
     }
@@ -267,8 +272,7 @@ __global__ __launch_bounds__(THREADS, !VEC ? 2 : sizeof(T) == 2 ? 4 : 3) void qk
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float ya = na[i], yb = nb[i];
-        na[i] = ya * c[i] + yb * s[i];
-        nb[i] = yb * c[i] - ya * s[i];
+        at.turn(i, ya, yb, c[i], -s[i], na[i], nb[i]);
         ss += a[i] * a[i] + b[i] * b[i];
         dot += na[i] * wa[i] * a[i] + nb[i] * wb[i] * b[i];
       }

@@ -226,3 +226,28 @@ def test_the_norm_alone_needs_no_positions(dim, rows):
     assert_fp32_close(got[4].cpu(), rw, "gradient of the gain of q")
     inside = both(torch.empty(50, 0, device=DEV), pos)
     assert all(torch.equal(a, b) for a, b in zip(got, inside))
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,rot", [(64, 32), (64, 0), (22, 10)])
+def test_elements_that_are_passed_on_stay_by_themselves(dim, rot, interleaved):
+    """What is not finite in one element that is not turned shows in that element alone: a gain there, and a gradient in the sums of
+    the gains' gradients (the head's own gradient has a mean over all of it)."""
+    q, k, dq, dk, wq, wk, cos, sin, pos = [x.to(DEV) for x in _case(4, 2, 1, dim, rot, torch.float32)]
+    ws = torch.empty(mlc.muloco_qk_norm_rope_workspace_bytes(dim), dtype=torch.uint8, device=DEV)
+    hp = mlc.QKNormRopeHParams(interleaved=interleaved)
+    for at in (rot, rot + 3, dim - 1):
+        rest = [i for i in range(dim) if i != at]
+        for bad in (float("inf"), float("nan")):
+            w = wq.clone()
+            w[at] = bad
+            out, clean = [torch.empty_like(q) for _ in range(2)], torch.empty_like(k)
+            mlc.muloco_qk_norm_rope(q, k, w, wk, cos, sin, pos, out[0], clean, hp)
+            mlc.muloco_qk_norm_rope(q, k, wq, wk, cos, sin, pos, out[1], clean, hp)
+            assert not torch.isfinite(out[0][..., at]).any() and torch.equal(out[0][..., rest], out[1][..., rest]), at
+            dy = dq.clone()
+            dy[1, 1, at] = bad
+            grads = [[torch.empty_like(q), torch.empty_like(k), torch.empty(dim, device=DEV), torch.empty(dim, device=DEV)] for _ in range(2)]
+            mlc.muloco_qk_norm_rope_backward(dy, dk, q, k, wq, wk, cos, sin, pos, *grads[0], ws, hp)
+            mlc.muloco_qk_norm_rope_backward(dq, dk, q, k, wq, wk, cos, sin, pos, *grads[1], ws, hp)
+            assert not torch.isfinite(grads[0][2][at]) and torch.equal(grads[0][2][rest], grads[1][2][rest]), at
