@@ -356,7 +356,8 @@ int muloco_adamw8_values(const mlc_adamw8_group* groups, int n_groups, float* co
  *
  * mlc_heads: [tokens][heads][head_dim], the last dimension contiguous, the other strides (in elements) free: slices of a
  * fused projection, or any order of tokens and heads.  An output may be the input of the same shape and strides
- * (each head is read before it is written); otherwise outputs overlap nothing.  k_heads may be 0 (k is
+ * (each head is read before it is written); otherwise outputs overlap nothing, nor may an output's own heads: the smaller of its
+ * strides is at least head_dim, the larger one spans all that the smaller one goes through.  k_heads may be 0 (k is
  * then not looked at; dk_gain, if not NULL, becomes 0); tokens may be 0.  head_dim and rot_dim are even, head_dim at
  * most 512, q_heads and k_heads at most 1024.
  */

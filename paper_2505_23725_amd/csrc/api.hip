@@ -1026,8 +1026,14 @@ static int check_heads(const mlc_qk_norm_rope* p, const mlc_heads* h, int heads,
   if (!heads) return MLC_OK;
   if (!h || (p->tokens && !h->ptr)) return MLC_ERR_NULL;
   if ((uintptr_t)h->ptr % elem_size(p->dtype) || h->token_stride < 0 || h->head_stride < 0) return MLC_ERR_ARG;
-  // two heads of an output may not lie on each other
-  if (output && ((heads > 1 && h->head_stride < p->head_dim) || (p->tokens > 1 && h->token_stride < p->head_dim))) return MLC_ERR_ARG;
+  // Two heads of an output may not lie on each other: the smaller of the two strides spans a head, the larger one all heads that
+  // the smaller one goes through.
+  if (output && p->tokens) {
+    struct Axis { int64_t stride, n; } in{h->head_stride, heads}, out{h->token_stride, p->tokens};
+    if (in.n == 1 || (out.n > 1 && out.stride < in.stride)) std::swap(in, out);
+    if (in.n > 1 && in.stride < p->head_dim) return MLC_ERR_ARG;
+    if (out.n > 1 && out.stride < (__int128)in.stride * (in.n - 1) + p->head_dim) return MLC_ERR_ARG;
+  }
   return MLC_OK;
 }
 static QkRows qk_rows(const mlc_heads* h, int heads) {

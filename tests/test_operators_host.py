@@ -168,3 +168,17 @@ def test_positions_are_not_needed_where_nothing_is_turned(back):
     heads = dict(heads={"dq_out" if back else "q": [P + 1, 192, 64]})
     assert _qk(back, change=dict(rot_dim=0, positions=None, cos=None, sin=None), **heads) == ARG
     assert _qk(back, change=dict(positions=None), **heads) == NULL
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("tokens,heads,token_stride,head_stride,fine", [
+    (4, 2, 64, 64, False),            # head 1 of a token is head 0 of the next
+    (4, 2, 127, 64, False), (4, 2, 128, 64, True), (4, 2, 128, 65, False), (4, 2, 129, 65, True), (4, 2, 64, 255, False), (4, 2, 64, 256, True),
+    (4, 3, 0, 1 << 20, False), (1, 3, 0, 64, True), (1, 3, 0, 63, False), (4, 1, 64, 0, True), (4, 1, 63, 0, False), (1, 1, 0, 0, True),
+    (2, 2, 1 << 62, 1 << 62, False), (1 << 40, 2, 1 << 62, 64, True), (1 << 40, 2, 64, 1 << 46, True), (1 << 40, 2, 64, (1 << 46) - 1, False),
+    (1 << 40, 2, 1 << 61, 1 << 62, False)])
+def test_heads_of_an_output_may_not_overlap(tokens, heads, token_stride, head_stride, fine, back):
+    """(what is fine goes on to the next tensor, which is missing)"""
+    first, second = ("dq", "dk") if back else ("q_out", "k_out")
+    got = _qk(back, change=dict(tokens=tokens, q_heads=heads), heads={first: [P, token_stride, head_stride], second: None})
+    assert got == (NULL if fine else ARG)
