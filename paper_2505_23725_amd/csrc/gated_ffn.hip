@@ -93,7 +93,6 @@ __device__ __forceinline__ void each(F&& f) { each_of(std::make_integer_sequence
 // (the hardware's reciprocal, an ulp of fp32 off: all of this is rounded to bf16 next)
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
 constexpr float GELU_C = 0.7978845608028654f, GELU_A = 0.044715f;
-__device__ __forceinline__ float tanh_of(float x) { return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __expf(2.f * x)); }
 // act(g) and act'(g)
 template <int ACT>
 __device__ __forceinline__ void activation(float g, float& a, float& da) {
@@ -102,9 +101,10 @@ __device__ __forceinline__ void activation(float g, float& a, float& da) {
     a = g * s;
     da = s + (a - a * s);
   } else {
-    const float th = tanh_of(GELU_C * (g + GELU_A * g * g * g));
-    a = 0.5f * g * (1.f + th);
-    da = 0.5f * (1.f + th) + 0.5f * g * (1.f - th * th) * GELU_C * (1.f + 3.f * GELU_A * g * g);
+    // 1/2 (1 + tanh(x)) = sigmoid(2 x), whose relative error stays an ulp or two where 1 + tanh(x) cancels
+    const float s = sigmoid(2.f * GELU_C * (g + GELU_A * g * g * g));
+    a = g * s;
+    da = s + a * (1.f - s) * (2.f * GELU_C) * (1.f + 3.f * GELU_A * g * g);
   }
 }
 
