@@ -1,6 +1,6 @@
 """One transformer layer trained with this library: the q/k norm with rotary positions and the gated feed-forward block make
 the gradients, Muon steps the matrices, AdamW with 8-bit states the embedding and the gains, and every few steps the DiLoCo outer
-step brings two resident workers together.
+step brings two resident workers together: all their parameters are the same after it.
 
     python examples/train_layer.py [--steps 40] [--width 256] [--hidden 704] [--tokens 512]
 
@@ -108,7 +108,8 @@ def train(steps=40, width=256, hidden=704, tokens=512, vocab=128, head_dim=64, e
     angle = torch.arange(length, device=device)[:, None] * 1e4 ** (-torch.arange(half, device=device) / half)
     tables = angle.cos().contiguous(), angle.sin().contiguous()
     replicas = [init(vocab, width, hidden, head_dim, device) for _ in range(workers)]
-    shared = {k: replicas[0][k].detach().float() for k in MATRICES}                # the global copy and its momentum
+    flat = lambda v: v.detach().view(-1, v.shape[-1])  # noqa: E731  (gains are matrices of one row to the outer step)
+    shared = {k: flat(v).float().clone() for k, v in replicas[0].items()}          # the global copy and its momentum
     outer = {k: torch.zeros_like(v) for k, v in shared.items()}
     momenta = [{k: torch.zeros_like(shared[k]) for k in MATRICES} for _ in replicas]
     states = [{k: mlc.adamw8_state(v) for k, v in p.items() if k not in MATRICES} for p in replicas]
@@ -134,7 +135,7 @@ def train(steps=40, width=256, hidden=704, tokens=512, vocab=128, head_dim=64, e
             if rank == 0:
                 losses.append(loss.detach())
         if step % every == 0:
-            mlc.muloco_outer_step([mlc.OuterGroup([p[k].detach() for p in replicas], shared[k], outer[k]) for k in MATRICES],
+            mlc.muloco_outer_step([mlc.OuterGroup([flat(p[k]) for p in replicas], shared[k], outer[k]) for k in shared],
                                   mlc.OuterHParams(K=workers, eta_out=0.7, mu=0.6))
             log(f"step {step}: loss {losses[-1].item():.4f}")
     return torch.stack(losses).tolist()

@@ -51,3 +51,31 @@ def test_gradients_against_plain_torch(monkeypatch):
     for k in p:
         err = ((grads[k].float() - refs[k].float()).norm() / refs[k].float().norm()).item()
         assert err < 3e-2, (k, err)
+
+
+def test_workers_are_one_model_after_an_outer_step(monkeypatch):
+    """Each worker goes its own way on its own data, in every parameter, until the outer step, and both learn."""
+    replicas, losses, met = [], [], []
+    init, loss_of, outer = layer.init, layer.loss_of, layer.mlc.muloco_outer_step
+
+    def kept(*args):
+        replicas.append(init(*args))
+        return replicas[-1]
+
+    def noted(*args):
+        loss = loss_of(*args)
+        losses.append(loss.item())
+        return loss
+
+    def joined(groups, hp):
+        assert not any(torch.equal(replicas[0][k], replicas[1][k]) for k in replicas[0])
+        outer(groups, hp)
+        assert [k for k in replicas[0] if not torch.equal(replicas[0][k], replicas[1][k])] == []
+        met.append(len(losses) // 2)
+    monkeypatch.setattr(layer, "init", kept)
+    monkeypatch.setattr(layer, "loss_of", noted)
+    monkeypatch.setattr(layer.mlc, "muloco_outer_step", joined)
+    layer.train(steps=30, log=lambda s: None)
+    assert met == [10, 20, 30] and len(losses) == 60
+    for rank in (0, 1):
+        assert losses[rank] > 0.8 * math.log(128) and losses[58 + rank] < 0.5 * losses[rank], (rank, losses[rank], losses[58 + rank])
