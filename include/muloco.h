@@ -314,8 +314,11 @@ int muloco_adamw_step(const mlc_adamw_group* groups, int n_groups, const mlc_ada
  *     theta <- theta - lr * (m c1) / (sqrt(v) c2 + eps) - lr * weight_decay * theta
  * with m and v as computed here, before they become codes.  The code of a value x is that of
  * fl(|x| fl(1 / scale)): the bits of that number plus r, cut to three bits of mantissa, where r is half a step
- * (dither = 0: to the nearest, halves away from 0) or uniform over a step (dither = 1: exact on average; r depends
- * on seed, block and element alone, so the caller gives every step another seed).  A v > 0 keeps a code > 0.
+ * (dither = 0) or uniform over a step (dither = 1; r depends on seed, block and element alone, so the caller gives every step another
+ * seed, and tensors that are not to be rounded alike each a call of their own).  A v > 0 keeps a code > 0.  So a number from the first
+ * level on, 1.125 2^-15 of the scale for m and 1.125 2^-31 for v, goes to the nearest level, halves away from 0, or to one of its two
+ * neighbours so that it is exact on average.  Below the first level it is neither: m becomes 0 below 1.0625 2^-15, or with
+ * dither up to 2^-15 always and from there to the first level with a probability that falls evenly to 0, and v the first level.
  * A gradient that is not finite makes its element, its block's scales and with them its block not finite.
  *
  * Any alignment that the element type has is accepted (codes: any, scales: 4 bytes).  Tensors of one dtype pair

@@ -594,7 +594,8 @@ def _adamw8_array(tensors: Sequence[tuple]):
 
 def muloco_adamw8_step(tensors: Sequence[tuple], hp: AdamWHParams, seed: Optional[int] = None, stream=None) -> None:
     """tensors: (param, grad, codes of m, codes of v, scales) tuples, see adamw8_state.  States are rounded to the nearest
-    code, or, with a seed (a new one every step), up or down by chance so that they are exact on average."""
+    code, or, with a seed (a new one every step), up or down by chance so that they are exact on average: both from the format's
+    first level on, 1.125 2^-15 (m) and 1.125 2^-31 (v) of a block's largest.  Tensors of one call are rounded alike, block by block."""
     chp = _AdamWHParams(hp.lr, hp.beta1, hp.beta2, hp.eps, hp.weight_decay, int(hp.bias_correction), int(hp.step))
     rc = library().muloco_adamw8_step(_adamw8_array(tensors), len(tensors), C.byref(chp), int(seed is not None),
                                       (0 if seed is None else int(seed)) & 0xffffffff, _stream(stream))

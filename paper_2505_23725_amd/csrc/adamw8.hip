@@ -5,17 +5,19 @@
 //
 // A tensor's elements, in their order in memory, form blocks of 256 that share two fp32 scales, the block's largest |m| and
 // largest v.  A code is a small floating-point number relative to the scale: for m a sign, four exponent and three
-// mantissa bits (2^-15 .. 1, and 0), for v, which is never negative but spans the square of the range, five exponent
-// and three mantissa bits (2^-31 .. 1, and 0).  Evenly spaced levels would send the smaller half of a block's second
-// moments to 0 and their steps to m / eps; here a v > 0 keeps at least the smallest code, so sqrt(v) >= 2^-15.5 of the
-// block's largest and m, which is 0 below 2^-15.9 of its largest, cannot outgrow it.  The largest element's code stands for
+// mantissa bits (1.125 2^-15 .. 1, and 0), for v, which is never negative but spans the square of the range, five exponent
+// and three mantissa bits (1.125 2^-31 .. 1, and 0).  Evenly spaced levels would send the smaller half of a block's second
+// moments to 0 and their steps to m / eps; here a v > 0 keeps at least the smallest code, so sqrt(v) >= 2^-15.4 of the
+// block's largest and m, which is 0 below 2^-14.9 of its largest, cannot outgrow it.  The largest element's code stands for
 // exactly the scale, so a block's magnitude follows its moving average without rounding.
 //
-// Rounding: to the nearest code, or (with a seed) up with the probability that makes the mean exact.  To the nearest, an
-// average that moves by less than half a step of its code (1 / 16 of its value) stands still next to its
-// block's largest; with rounding by chance it moves at the right rate on average.  The 20 bits per element come from a
+// Rounding, from the first level on: to the nearest code, or (with a seed) up with the probability that makes the mean exact.  To the
+// nearest, an average that moves by less than half a step of its code (1 / 16 of its value) stands still next to its
+// block's largest; with rounding by chance it moves at the right rate on average.  Below the first level neither holds: an m up to
+// 2^-15 of its block's largest becomes 0 whatever the seed (so an element with gradients that small beside an outlier's is moved by
+// nothing but weight decay), and a v > 0 becomes the first level.  The 20 bits per element come from a
 // hash of (seed, block), moved on by an odd constant from element to element: one hash per block, and over the steps every
-// element's sequence is as the hash's.
+// element's sequence is as the hash's.  (A tensor's blocks count from 0: tensors of one call share their blocks' hashes.)
 //
 // All sums and products of the states are single fp32 operations in a fixed order (no contraction), so that codes are
 // reproducible bit for bit.
