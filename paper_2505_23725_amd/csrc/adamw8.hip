@@ -15,7 +15,7 @@
 // nearest, an average that moves by less than half a step of its code (1 / 16 of its value) stands still next to its
 // block's largest; with rounding by chance it moves at the right rate on average.  Below the first level neither holds: an m up to
 // 2^-15 of its block's largest becomes 0 whatever the seed (so an element with gradients that small beside an outlier's is moved by
-// nothing but weight decay), and a v > 0 becomes the first level.  The 20 bits per element come from a
+// its newest gradient's part of the average alone), and a v > 0 becomes the first level.  The 20 bits per element come from a
 // hash of (seed, block), moved on by an odd constant from element to element: one hash per block, and over the steps every
 // element's sequence is as the hash's.  (A tensor's blocks count from 0: tensors of one call share their blocks' hashes.)
 //
