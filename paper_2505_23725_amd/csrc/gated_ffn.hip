@@ -26,12 +26,12 @@
 #include <utility>
 
 #include "common.h"
+#include "ffn_plan.h"
 #include "mfma_tile.h"
 
 namespace mlc {
 namespace {
 
-constexpr int BK = 64;
 constexpr int NTHREADS = 256;
 constexpr int NUM_XCD = 8;
 constexpr int GROUP_M = 8;                          // tile rows per group of the tile order
@@ -695,15 +695,6 @@ __global__ __launch_bounds__(NTHREADS) void ffn_join_kernel(GemmArgs g) {
 
 int check_launch() { return hipGetLastError() == hipSuccess ? MLC_OK : MLC_ERR_LAUNCH; }
 
-// Whether M tokens take that kernel for a product with N x K weights.  Every workgroup reads all of x, so that beside the weights
-// the L2 serves as much again for every 16 tokens: to 8 tokens that is hidden (2048 / 5632, both products: 23.3 us for one
-// token, 24.5 for eight; the tiles 26.1 and 26.3), and of small weights, whose time is the launches', to 32 (512 / 2048, 16 tokens:
-// 12.8 and 17.7; 2048 / 5632, 16 and 32 tokens: 27.8 and 35.2, the tiles 26.5 and 27.2).  Few rows of long weights are too
-// few workgroups (20480 / 64, one token: 27 us, cut tiles 21).
-bool few(int64_t M, int64_t N, int64_t K) {
-  if (N < 512 && K > 4096) return false;
-  return M <= 8 || (M <= 32 && N * K <= (int64_t)1 << 21);
-}
 template <bool DUAL, int ACT>
 int launch_few(const bf16_t* x, const bf16_t* w0, const bf16_t* w1, int64_t M, int64_t N, int64_t K, bf16_t* out, bf16_t* gate,
                bf16_t* up, hipStream_t stream) {
@@ -720,12 +711,6 @@ int launch_few(const bf16_t* x, const bf16_t* w0, const bf16_t* w1, int64_t M, i
 #undef MLC_FEW
   return check_launch();
 }
-
-constexpr int UNITS = 256;                          // compute units
-// per_unit: workgroups a compute unit: one, whose ring fills its LDS (with a small tile four K tiles ahead), or two with half of
-// it each.
-struct Plan { int bm, bn, per_unit, whole, splits; };
-struct Size { int64_t M, N; };                      // of a product; N: columns of accumulators (2 f of UP)
 
 template <int FORM, int ACT, int BM, int BN, int NB>
 int launch_tile(GemmArgs& g, const Plan& plan, double flops, double bytes, hipStream_t stream) {
@@ -779,51 +764,6 @@ int launch_form(GemmArgs& g, const Plan& plan, hipStream_t stream) {
   return launch_tile<FORM, ACT, 64, 128, 5>(g, plan, flops, bytes, stream);
 }
 
-// The tile, and whether the tiles of the last, partly filled round are cut along K (only where can_split), by an estimate of the
-// time: the compute units' share of tiles times what a tile's kt K tiles and its ends take, and the joining of cut tiles.
-// The constants are fitted to the block's times on 13 shapes from 77 x 2560 x 10240 to 8192 x 2048 x 5632, each form's tile and
-// cuts varied with the others held: the choice takes 1.065 of the best one's time at most, over 1.02 in three of 65 (one tile
-// for all: 1.5 times and more in some of them).  `few` and `all`: a K tile's time with few tiles and with every unit busy,
-// all[0] of products whose operands are both K-contiguous (UP, NT), all[1] with K-strided ones; in between by the units that
-// have work, and of two workgroups a unit once there are two.
-struct TileCost { int bm, bn, per_unit; double few, all[2], ends; };      // us
-constexpr TileCost TILE_COSTS[] = {{256, 256, 1, 0.76, {1.20, 1.10}, 9.9}, {128, 128, 1, 0.53, {0.42, 0.43}, 3.1},
-                                   {128, 128, 2, 0.51, {0.39, 0.37}, 2.6}, {64, 128, 1, 0.42, {0.45, 0.35}, 2.4},
-                                   {64, 128, 2, 0.54, {0.33, 0.32}, 1.9}};
-constexpr double JOIN = 7.4, JOIN_BYTES = 3.7e6;    // us, and bytes a us
-Plan pick(const Size* s, int n, int64_t kt, bool strided, bool can_split) {
-  Plan best{};
-  double least = 1e300;
-  for (const TileCost& c : TILE_COSTS) {
-    int64_t tiles = 0;
-    for (int i = 0; i < n; ++i) tiles += ((s[i].M + c.bm - 1) / c.bm) * ((s[i].N + c.bn - 1) / c.bn);
-    const int64_t slots = (int64_t)UNITS * c.per_unit, rest = tiles % slots, whole = tiles - rest;
-    const double full = (double)(whole / UNITS) * (kt * c.all[strided] + c.ends);
-    for (int splits = 1; splits <= 16; ++splits) {
-      if (splits > 1 && (!can_split || rest * splits > slots || kt / splits < 4)) break;
-      const int64_t items = rest * splits, share = (items + UNITS - 1) / UNITS;
-      const double busy = c.per_unit == 2 ? share > 1 : items < UNITS ? (double)items / UNITS : 1.0;
-      const double k_time = c.few + (c.all[strided] - c.few) * busy;
-      const double join = splits > 1 ? JOIN + (double)items * c.bm * c.bn * 8 / JOIN_BYTES : 0.0;
-      const double t = full + (double)share * ((double)kt / splits * k_time + c.ends) + join;
-      if (t < least) {
-        least = t;
-        best = Plan{c.bm, c.bn, c.per_unit, splits > 1 ? (int)whole : 0, splits};
-      }
-    }
-  }
-  return best;
-}
-// (at most one round of items are split ones)
-size_t partial_bytes(const Plan& p) { return p.splits > 1 ? (size_t)UNITS * p.per_unit * p.bm * p.bn * 4 : 0; }
-
-int64_t k_tiles(int64_t K) { return (K + BK - 1) / BK; }
-Plan plan_up(const FfnShape& s) { const Size z{s.t, 2 * s.f}; return pick(&z, 1, k_tiles(s.d), false, false); }
-Plan plan_down(const FfnShape& s) { const Size z{s.t, s.d}; return pick(&z, 1, k_tiles(s.f), false, true); }
-Plan plan_inner(const FfnShape& s) { const Size z{s.t, s.f}; return pick(&z, 1, k_tiles(s.d), true, false); }
-Plan plan_dx(const FfnShape& s) { const Size z{s.t, s.d}; return pick(&z, 1, 2 * k_tiles(s.f), true, true); }
-Plan plan_dw(const FfnShape& s) { const Size z[3] = {{s.f, s.d}, {s.f, s.d}, {s.d, s.f}}; return pick(z, 3, k_tiles(s.t), true, true); }
-
 Problem problem(const bf16_t* A, long lda, const bf16_t* B, long ldb, bf16_t* D, long ldd, int64_t M, int64_t N, int64_t K) {
   Problem p{};
   p.A[0] = A; p.B[0] = B; p.lda = lda; p.ldb = ldb; p.D = D; p.ldd = ldd;
@@ -833,9 +773,9 @@ Problem problem(const bf16_t* A, long lda, const bf16_t* B, long ldb, bf16_t* D,
 
 }  // namespace
 
-size_t ffn_forward_workspace(const FfnShape& s) { return few(s.t, s.d, s.f) ? 0 : partial_bytes(plan_down(s)); }
+size_t ffn_forward_workspace(const FfnShape& s) { return few(s.t, s.d, s.f) ? 0 : partial_bytes(plan_down(s.t, s.d, s.f)); }
 size_t ffn_backward_workspace(const FfnShape& s) {
-  const size_t dx = partial_bytes(plan_dx(s)), dw = partial_bytes(plan_dw(s));
+  const size_t dx = partial_bytes(plan_dx(s.t, s.d, s.f)), dw = partial_bytes(plan_dw(s.t, s.d, s.f));
   return 2 * (size_t)round_up(s.t * s.f * 2, 256) + (dx > dw ? dx : dw);
 }
 
@@ -852,7 +792,7 @@ int launch_ffn_forward(const FfnShape& s, const bf16_t* x, const bf16_t* wg, con
     g.p[0] = problem(x, s.d, wg, s.d, hidden, s.f, s.t, s.f, s.d);
     g.p[0].B[1] = wu;
     g.gate = gate; g.up = up;
-    const Plan both = plan_up(s);
+    const Plan both = plan_up(s.t, s.d, s.f);
     rc = silu ? launch_form<UP, MLC_ACT_SILU>(g, both, stream) : launch_form<UP, MLC_ACT_GELU_TANH>(g, both, stream);
   }
   if (rc != MLC_OK) return rc;
@@ -861,7 +801,7 @@ int launch_ffn_forward(const FfnShape& s, const bf16_t* x, const bf16_t* wg, con
   n.problems = 1;
   n.p[0] = problem(hidden, s.f, wd, s.f, y, s.d, s.t, s.d, s.f);
   n.partial = (float*)workspace;
-  return launch_form<NT>(n, plan_down(s), stream);
+  return launch_form<NT>(n, plan_down(s.t, s.d, s.f), stream);
 }
 
 int launch_ffn_backward(const FfnShape& s, const bf16_t* dy, const bf16_t* x, const bf16_t* wg, const bf16_t* wu, const bf16_t* wd,
@@ -876,7 +816,7 @@ int launch_ffn_backward(const FfnShape& s, const bf16_t* dy, const bf16_t* x, co
     g.problems = 1;
       g.p[0] = problem(dy, s.d, wd, s.f, dg, s.f, s.t, s.f, s.d);
     g.gate = const_cast<bf16_t*>(gate); g.up = const_cast<bf16_t*>(up); g.du = du;
-    const Plan inner = plan_inner(s);
+    const Plan inner = plan_inner(s.t, s.d, s.f);
     rc = launch_form<DH>(g, inner, stream);
     if (rc != MLC_OK) return rc;
     GemmArgs n{};
@@ -884,7 +824,7 @@ int launch_ffn_backward(const FfnShape& s, const bf16_t* dy, const bf16_t* x, co
     n.p[0] = problem(dg, s.f, wg, s.d, dx, s.d, s.t, s.d, s.f);
     n.p[0].A[1] = du; n.p[0].B[1] = wu;
     n.partial = partial;
-    rc = launch_form<NN>(n, plan_dx(s), stream);
+    rc = launch_form<NN>(n, plan_dx(s.t, s.d, s.f), stream);
     if (rc != MLC_OK) return rc;
   }
   GemmArgs w{};
@@ -893,7 +833,7 @@ int launch_ffn_backward(const FfnShape& s, const bf16_t* dy, const bf16_t* x, co
   w.p[1] = problem(du, s.f, x, s.d, dwu, s.d, s.f, s.d, s.t);
   w.p[2] = problem(dy, s.d, hidden, s.f, dwd, s.f, s.d, s.f, s.t);
   w.partial = partial;
-  return launch_form<TN>(w, plan_dw(s), stream);
+  return launch_form<TN>(w, plan_dw(s.t, s.d, s.f), stream);
 }
 
 }  // namespace mlc
