@@ -394,9 +394,11 @@ int muloco_qk_norm_rope_backward(const mlc_qk_norm_rope* p, const mlc_heads* dq_
  *
  *     g = x Wg^T ; u = x Wu^T ; h = act(g) u ; y = h Wd^T
  * x, y [tokens][d]; w_gate, w_up [f][d]; w_down [d][f] (the shapes that muloco_inner_step takes as d x f and f x d
- * matrices); hidden (h), gate and up [tokens][f].  Everything is contiguous bf16, 16-byte aligned, d and f are
- * multiples of 8; products run on the bf16 matrix cores with fp32 sums.  hidden is rounded to bf16 before the
- * second product, and so are gate and up and, backwards, the gradients of g and u: results carry a few bf16 roundings.
+ * matrices); hidden (h), gate and up [tokens][f].  Everything is contiguous bf16 (gate and up fp32 with factors_32bit), 16-byte
+ * aligned, d and f are multiples of 8; products run on the bf16 matrix cores with fp32 sums.  hidden is rounded to bf16 before the
+ * second product, and so are, backwards, gate and up (unless factors_32bit) and the gradients of g and u.  Each such rounding is
+ * 1.7e-3 of a value in the mean, as the result's own is: relative to exact arithmetic y and the gradient of w_down carry 2.4e-3,
+ * the other gradients 2.9e-3, or 2.4e-3 with factors_32bit.
  * act: SiLU, g / (1 + e^-g), or the tanh form of GELU, g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))).
  *
  * Forward: gate and up receive what the backward call needs of the two projections, act(g) and u act'(g); they are both
@@ -414,6 +416,7 @@ typedef struct {
   const void* w_gate;
   const void* w_up;
   const void* w_down;
+  int factors_32bit;               /* gate and up are fp32, in both calls; 0: bf16          */
 } mlc_gated_ffn;
 
 size_t muloco_gated_ffn_workspace_bytes(int64_t tokens, int64_t d, int64_t f, int backward);

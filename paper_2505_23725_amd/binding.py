@@ -90,7 +90,7 @@ class _QKNormRope(C.Structure):
 
 class _GatedFFN(C.Structure):
     _fields_ = [("tokens", C.c_int64), ("d", C.c_int64), ("f", C.c_int64), ("act", C.c_int), ("x", C.c_void_p),
-                ("w_gate", C.c_void_p), ("w_up", C.c_void_p), ("w_down", C.c_void_p)]
+                ("w_gate", C.c_void_p), ("w_up", C.c_void_p), ("w_down", C.c_void_p), ("factors_32bit", C.c_int)]
 
 
 class _KernelTiming(C.Structure):
@@ -755,17 +755,29 @@ def _bf16_ptr(t: torch.Tensor, shape, what: str) -> int:
     return _dev_ptr(t, what)
 
 
+def _factor_ptrs(d: _GatedFFN, gate, up):
+    """Addresses of the factors, whose type goes into the description: both bf16 or both fp32."""
+    if gate.dtype == up.dtype == torch.float32:
+        d.factors_32bit = 1
+        for t, what in ((gate, "gate"), (up, "up")):
+            if tuple(t.shape) != (d.tokens, d.f):
+                raise ValueError(f"{what} must be {[d.tokens, d.f]}")
+        return _dev_ptr(gate, "gate"), _dev_ptr(up, "up")
+    return _bf16_ptr(gate, (d.tokens, d.f), "gate"), _bf16_ptr(up, (d.tokens, d.f), "up")
+
+
 def muloco_gated_ffn(x, w_gate, w_up, w_down, out, hidden, workspace: Optional[torch.Tensor] = None, act: str = "silu",
                      gate: Optional[torch.Tensor] = None, up: Optional[torch.Tensor] = None, stream=None) -> None:
     """out = (act(x w_gate^T) * (x w_up^T)) w_down^T.  hidden [tokens, f] receives the product in the brackets; gate and up (both
-    or neither) what the backward call needs of its factors: act(.) of the first, and act'(.) of it times the second."""
+    or neither) what the backward call needs of its factors: act(.) of the first, and act'(.) of it times the second, in bfloat16 or,
+    for a rounding fewer in the gradients, both in float32."""
     d = _ffn_desc(x, w_gate, w_up, w_down, act)
     inner = (d.tokens, d.f)
     if (gate is None) != (up is None):
         raise ValueError("gate and up: both or neither")
     ws, size = _workspace(workspace)
-    rc = library().muloco_gated_ffn(C.byref(d), None if gate is None else _bf16_ptr(gate, inner, "gate"),
-                                    None if up is None else _bf16_ptr(up, inner, "up"), _bf16_ptr(hidden, inner, "hidden"),
+    factors = (None, None) if gate is None else _factor_ptrs(d, gate, up)
+    rc = library().muloco_gated_ffn(C.byref(d), *factors, _bf16_ptr(hidden, inner, "hidden"),
                                     _bf16_ptr(out, (d.tokens, d.d), "out"), ws, size, _stream(stream))
     _check(rc, "muloco_gated_ffn")
 
@@ -776,8 +788,9 @@ def muloco_gated_ffn_backward(dout, x, w_gate, w_up, w_down, gate, up, hidden, d
     d = _ffn_desc(x, w_gate, w_up, w_down, act)
     inner, outer, fd, df = (d.tokens, d.f), (d.tokens, d.d), (d.f, d.d), (d.d, d.f)
     ws, size = _workspace(workspace)
+    factors = _factor_ptrs(d, gate, up)
     rc = library().muloco_gated_ffn_backward(
-        C.byref(d), _bf16_ptr(gate, inner, "gate"), _bf16_ptr(up, inner, "up"), _bf16_ptr(hidden, inner, "hidden"),
+        C.byref(d), *factors, _bf16_ptr(hidden, inner, "hidden"),
         _bf16_ptr(dout, outer, "dout"), _bf16_ptr(dx, outer, "dx"), _bf16_ptr(dw_gate, fd, "dw_gate"),
         _bf16_ptr(dw_up, fd, "dw_up"), _bf16_ptr(dw_down, df, "dw_down"), ws, size, _stream(stream))
     _check(rc, "muloco_gated_ffn_backward")

@@ -1102,14 +1102,14 @@ static int check_ffn_shape(int64_t tokens, int64_t d, int64_t f) {
 
 size_t muloco_gated_ffn_workspace_bytes(int64_t tokens, int64_t d, int64_t f, int backward) {
   if (check_ffn_shape(tokens, d, f) != MLC_OK) return 0;
-  const FfnShape s{tokens, d, f, 0};
+  const FfnShape s{tokens, d, f, 0, false};
   return backward ? ffn_backward_workspace(s) : ffn_forward_workspace(s);
 }
 
 // What holds a row per token may be missing where there are no tokens.
 static int check_ffn(const mlc_gated_ffn* p, const void* const* per_token, int n_token, const void* const* matrices, int n_matrices,
                      const void* workspace, size_t bytes, size_t needed) {
-  if (p->act != MLC_ACT_SILU && p->act != MLC_ACT_GELU_TANH) return MLC_ERR_ARG;
+  if ((p->act != MLC_ACT_SILU && p->act != MLC_ACT_GELU_TANH) || (p->factors_32bit != 0 && p->factors_32bit != 1)) return MLC_ERR_ARG;
   for (int i = 0; i < n_token; ++i) {
     if (p->tokens && !per_token[i]) return MLC_ERR_NULL;
     if (!aligned16(per_token[i])) return MLC_ERR_ARG;
@@ -1129,13 +1129,13 @@ int muloco_gated_ffn(const mlc_gated_ffn* p, void* gate, void* up, void* hidden,
   if (rc != MLC_OK) return rc;
   if (p->tokens && !gate != !up) return MLC_ERR_NULL;
   if (!aligned16(gate) || !aligned16(up)) return MLC_ERR_ARG;
-  const FfnShape s{p->tokens, p->d, p->f, p->act};
+  const FfnShape s{p->tokens, p->d, p->f, p->act, p->factors_32bit != 0};
   const void* const per_token[] = {p->x, hidden, y};
   const void* const matrices[] = {p->w_gate, p->w_up, p->w_down};
   rc = check_ffn(p, per_token, 3, matrices, 3, workspace, workspace_bytes, ffn_forward_workspace(s));
   if (rc != MLC_OK || !p->tokens) return rc;
   return launch_ffn_forward(s, (const bf16_t*)p->x, (const bf16_t*)p->w_gate, (const bf16_t*)p->w_up, (const bf16_t*)p->w_down,
-                            (bf16_t*)gate, (bf16_t*)up, (bf16_t*)hidden, (bf16_t*)y, workspace, (hipStream_t)stream_);
+                            gate, up, (bf16_t*)hidden, (bf16_t*)y, workspace, (hipStream_t)stream_);
 }
 
 int muloco_gated_ffn_backward(const mlc_gated_ffn* p, const void* gate, const void* up, const void* hidden, const void* dy, void* dx,
@@ -1143,13 +1143,13 @@ int muloco_gated_ffn_backward(const mlc_gated_ffn* p, const void* gate, const vo
   if (!p) return MLC_ERR_NULL;
   int rc = check_ffn_shape(p->tokens, p->d, p->f);
   if (rc != MLC_OK) return rc;
-  const FfnShape s{p->tokens, p->d, p->f, p->act};
+  const FfnShape s{p->tokens, p->d, p->f, p->act, p->factors_32bit != 0};
   const void* const per_token[] = {p->x, gate, up, hidden, dy, dx};
   const void* const matrices[] = {p->w_gate, p->w_up, p->w_down, dw_gate, dw_up, dw_down};
   rc = check_ffn(p, per_token, 6, matrices, 6, workspace, workspace_bytes, ffn_backward_workspace(s));
   if (rc != MLC_OK) return rc;
   return launch_ffn_backward(s, (const bf16_t*)dy, (const bf16_t*)p->x, (const bf16_t*)p->w_gate, (const bf16_t*)p->w_up,
-                             (const bf16_t*)p->w_down, (const bf16_t*)gate, (const bf16_t*)up, (const bf16_t*)hidden, (bf16_t*)dx,
+                             (const bf16_t*)p->w_down, gate, up, (const bf16_t*)hidden, (bf16_t*)dx,
                              (bf16_t*)dw_gate, (bf16_t*)dw_up, (bf16_t*)dw_down, workspace, (hipStream_t)stream_);
 }
 

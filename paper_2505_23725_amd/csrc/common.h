@@ -297,13 +297,13 @@ struct QkArgs {
 int launch_qk_norm_rope(QkArgs g, int dtype, int interleaved, bool backward, hipStream_t stream);
 
 // ---- gated feed-forward block (gated_ffn.hip) ----------------------------------------
-struct FfnShape { int64_t t, d, f; int act; };
+struct FfnShape { int64_t t, d, f; int act; bool wide; };       // wide: gate and up are fp32
 size_t ffn_forward_workspace(const FfnShape& s);
 size_t ffn_backward_workspace(const FfnShape& s);
-int launch_ffn_forward(const FfnShape& s, const bf16_t* x, const bf16_t* wg, const bf16_t* wu, const bf16_t* wd, bf16_t* gate, bf16_t* up,
+int launch_ffn_forward(const FfnShape& s, const bf16_t* x, const bf16_t* wg, const bf16_t* wu, const bf16_t* wd, void* gate, void* up,
                        bf16_t* hidden, bf16_t* y, void* workspace, hipStream_t stream);
 int launch_ffn_backward(const FfnShape& s, const bf16_t* dy, const bf16_t* x, const bf16_t* wg, const bf16_t* wu, const bf16_t* wd,
-                        const bf16_t* gate, const bf16_t* up, const bf16_t* hidden, bf16_t* dx, bf16_t* dwg, bf16_t* dwu, bf16_t* dwd,
+                        const void* gate, const void* up, const bf16_t* hidden, bf16_t* dx, bf16_t* dwg, bf16_t* dwu, bf16_t* dwd,
                         void* workspace, hipStream_t stream);
 
 // ---- outer step kernels (outer.hip) ----------------------------------------------

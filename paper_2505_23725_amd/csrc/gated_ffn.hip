@@ -14,7 +14,9 @@
 //   NN    dx: one sum over the 2 f columns of dg and du
 //   TN    the weights' gradients, three products in one launch
 // bf16 operands, fp32 sums.  h, the factors, dg and du are rounded to bf16 where they are stored (h, dg and du are the next
-// product's operands); all are formed from unrounded g and u.  The factors are kept instead of g and u because DH's epilogue has
+// product's operands); all are formed from unrounded g and u.  A caller who keeps the factors in fp32 (twice their memory) saves
+// one of the three roundings on the way to dx and the projections' gradients: relative to fp64 2.4e-3 instead of 2.9e-3, where one
+// rounding alone gives 1.7e-3 (16384 x 2048 x 5632: forward 840 -> 857 us, backward 1647 -> 1707).  The factors are kept instead of g and u because DH's epilogue has
 // the matrix cores wait for it: with the activation's slope in it (20 instructions an element, two of them quarter rate)
 // a tile of 256 x 256 took 24 us beside its 46 us of products.
 //
@@ -37,7 +39,7 @@ constexpr int NUM_XCD = 8;
 constexpr int GROUP_M = 8;                          // tile rows per group of the tile order
 constexpr unsigned int BUFFER_END = 0xfffffff0u;    // no buffer reaches it: a load there gives 0, a store is dropped
 constexpr int MAX_PROBLEMS = 3;
-enum Form { UP, NT, DH, NN, TN };
+enum Form { UP, NT, DH, NN, TN, UP32, DH32 };       // the last two: with fp32 factors
 
 struct Problem {
   const bf16_t* A[2]; const bf16_t* B[2];           // NN: of the two halves of the sum; UP: B of g and of u
@@ -52,7 +54,7 @@ struct GemmArgs {
   Problem p[MAX_PROBLEMS];
   int problems, tiles, whole, splits;
   float* partial;
-  bf16_t* gate; bf16_t* up;                         // act(g) and u act'(g); UP: out (may be null); DH: in
+  void* gate; void* up;                             // act(g) and u act'(g), bf16 or fp32; UP: out (may be null); DH: in
   bf16_t* du;                                       // DH: out
 };
 struct Place { int problem, m0, n0; };
@@ -129,8 +131,10 @@ struct Cursor {
 
 // Of a 128 x 128 or smaller tile the compiler's own MFMAs; the 256 x 256 one's are written out (see mfma_tile.h).
 // ACT: of UP.
-template <int FORM, int ACT, int BM, int BN, int NB>
+template <int KIND, int ACT, int BM, int BN, int NB>
 __global__ __launch_bounds__(NTHREADS, NB == 5 && BM != 256 ? 2 : 1) void ffn_gemm_kernel(GemmArgs g) {
+  constexpr bool WIDE = KIND == UP32 || KIND == DH32;
+  constexpr int FORM = KIND == UP32 ? UP : KIND == DH32 ? DH : KIND;
   constexpr bool AKS = FORM == TN, BKS = FORM == DH || FORM == NN || FORM == TN, DUAL = FORM == UP;
   constexpr int TI = BM / 32, TJ = BN / 32, NM = TI * TJ;
   constexpr int NCHA = BM / 32, NCHB = BN / 32;     // transfers per thread and buffer
@@ -460,6 +464,13 @@ __global__ __launch_bounds__(NTHREADS, NB == 5 && BM != 256 ? 2 : 1) void ffn_ge
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
   };
   auto rsrc_of = [&](const bf16_t* q) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(q) + origin, 0, BUFFER_END, 0x00020000); };
+  // the factors' buffers, and the places of 8 (4 fp32) of their elements there
+  constexpr int FACTOR = WIDE ? 2 : 1;              // times two bytes an element
+  auto rsrc_factor = [&](void* q) { return __builtin_amdgcn_make_buffer_rsrc((bf16_t*)q + origin * FACTOR, 0, BUFFER_END, 0x00020000); };
+  auto place_factor = [&](int row, int col) {
+    const unsigned int at = place(row, col);
+    return at == BUFFER_END ? BUFFER_END : at * FACTOR;
+  };
   auto store_row = [&](__amdgpu_buffer_rsrc_t r, int i, const u32x4 (&w)[JC]) {
     const int row = row_at(i);
     if constexpr (JC == 1) {
@@ -476,7 +487,7 @@ __global__ __launch_bounds__(NTHREADS, NB == 5 && BM != 256 ? 2 : 1) void ffn_ge
     }
   };
   if constexpr (FORM == UP) {
-    const __amdgpu_buffer_rsrc_t rh = rsrc_of(P.D), rg = rsrc_of(g.gate), ru = rsrc_of(g.up);
+    const __amdgpu_buffer_rsrc_t rh = rsrc_of(P.D), rg = rsrc_factor(g.gate), ru = rsrc_factor(g.up);
     auto all = [&](auto keep_tag) {                 // keep: the backward call's factors too
       constexpr bool KEEP = decltype(keep_tag)::value;
       each<TI>([&](auto row_tag) {
@@ -496,27 +507,48 @@ __global__ __launch_bounds__(NTHREADS, NB == 5 && BM != 256 ? 2 : 1) void ffn_ge
             u[x] *= da;
           }
           wh[J] = Vec8<bf16_t>::pack(h);
-          if (KEEP) { wg[J] = Vec8<bf16_t>::pack(v); wu[J] = Vec8<bf16_t>::pack(u); }
+          if (KEEP && !WIDE) { wg[J] = Vec8<bf16_t>::pack(v); wu[J] = Vec8<bf16_t>::pack(u); }
+          if constexpr (KEEP && WIDE) {
+            const unsigned int at = place_factor(row_at(i), col0 + 32 * J), next = at == BUFFER_END ? at : at + 16;
+            auto four = [](const float* q) { return u32x4{__float_as_uint(q[0]), __float_as_uint(q[1]), __float_as_uint(q[2]), __float_as_uint(q[3])}; };
+            __builtin_amdgcn_raw_buffer_store_b128(four(v), rg, at, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(four(v + 4), rg, next, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(four(u), ru, at, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(four(u + 4), ru, next, 0, 0);
+          }
         }
         store_row(rh, i, wh);
-        if (KEEP) {
+        if (KEEP && !WIDE) {
           store_row(rg, i, wg);
           store_row(ru, i, wu);
         }
         __builtin_amdgcn_sched_barrier(0);
       });
     };
-    if (g.gate) all(std::true_type{});
+    if constexpr (WIDE) all(std::true_type{});
+    else if (g.gate) all(std::true_type{});
     else all(std::false_type{});
   } else if constexpr (FORM == DH) {
-    const __amdgpu_buffer_rsrc_t rd = rsrc_of(P.D), rdu = rsrc_of(g.du), rg = rsrc_of(g.gate), ru = rsrc_of(g.up);
-    u32x4 gt[2][JC], up[2][JC];                     // this row's and the next one's
+    const __amdgpu_buffer_rsrc_t rd = rsrc_of(P.D), rdu = rsrc_of(g.du), rg = rsrc_factor(g.gate), ru = rsrc_factor(g.up);
+    u32x4 gt[2][JC * FACTOR], up[2][JC * FACTOR];   // this row's and the next one's
     auto fetch = [&](int i) {
 #pragma unroll
       for (int J = 0; J < JC; ++J) {
-        const unsigned int at = place(row_at(i), col0 + 32 * J);
-        gt[i & 1][J] = __builtin_amdgcn_raw_buffer_load_b128(rg, at, 0, 0);
-        up[i & 1][J] = __builtin_amdgcn_raw_buffer_load_b128(ru, at, 0, 0);
+        const unsigned int at = place_factor(row_at(i), col0 + 32 * J);
+#pragma unroll
+        for (int half = 0; half < FACTOR; ++half) {
+          const unsigned int there = half && at != BUFFER_END ? at + 16 : at;
+          gt[i & 1][J * FACTOR + half] = __builtin_amdgcn_raw_buffer_load_b128(rg, there, 0, 0);
+          up[i & 1][J * FACTOR + half] = __builtin_amdgcn_raw_buffer_load_b128(ru, there, 0, 0);
+        }
+      }
+    };
+    auto factors = [&](const u32x4* w, float (&f)[8]) {
+      if constexpr (WIDE) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) f[x] = __uint_as_float(w[x / 4][x % 4]);
+      } else {
+        Vec8<bf16_t>::unpack(w[0], f);
       }
     };
     fetch(0);
@@ -529,8 +561,8 @@ __global__ __launch_bounds__(NTHREADS, NB == 5 && BM != 256 ? 2 : 1) void ffn_ge
       for (int J = 0; J < JC; ++J) {
         float v[8], gv[8], uv[8];
         take(i, J, v);
-        Vec8<bf16_t>::unpack(gt[i & 1][J], gv);
-        Vec8<bf16_t>::unpack(up[i & 1][J], uv);
+        factors(&gt[i & 1][J * FACTOR], gv);
+        factors(&up[i & 1][J * FACTOR], uv);
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
           gv[x] *= v[x];
@@ -586,9 +618,9 @@ __global__ __launch_bounds__(NTHREADS, NB == 5 && BM != 256 ? 2 : 1) void ffn_ge
 // loads under way (16 bytes a lane each), and there are enough wavefronts a workgroup that a few hundred rows of
 // weights keep the chip's memory busy.
 constexpr int STEPS = 4;                            // MFMA steps of 32 k in a piece
-template <bool DUAL, int ACT, int TM>
+template <bool DUAL, int ACT, int TM, bool WIDE>
 __global__ __launch_bounds__(1024) void ffn_few_kernel(const bf16_t* x, const bf16_t* w0, const bf16_t* w1, int M, int N, int K,
-                                                       bf16_t* out, bf16_t* gate, bf16_t* up) {
+                                                       bf16_t* out, void* gate, void* up) {
   constexpr int NW = DUAL ? 2 : 1;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   f32x4* const held = (f32x4*)smem;                 // [wavefront][TM][NW][lane]
@@ -663,9 +695,12 @@ __global__ __launch_bounds__(1024) void ffn_few_kernel(const bf16_t* x, const bf
         v[1][c] *= da;
       }
       put(out, h);
-      if (gate) {
-        put(gate, v[0]);
-        put(up, v[1]);
+      if constexpr (WIDE) {
+        *reinterpret_cast<f32x4*>((float*)gate + at) = v[0];
+        *reinterpret_cast<f32x4*>((float*)up + at) = v[1];
+      } else if (gate) {
+        put((bf16_t*)gate, v[0]);
+        put((bf16_t*)up, v[1]);
       }
     } else {
       put(out, v[0]);
@@ -695,9 +730,9 @@ __global__ __launch_bounds__(NTHREADS) void ffn_join_kernel(GemmArgs g) {
 
 int check_launch() { return hipGetLastError() == hipSuccess ? MLC_OK : MLC_ERR_LAUNCH; }
 
-template <bool DUAL, int ACT>
-int launch_few(const bf16_t* x, const bf16_t* w0, const bf16_t* w1, int64_t M, int64_t N, int64_t K, bf16_t* out, bf16_t* gate,
-               bf16_t* up, hipStream_t stream) {
+template <bool DUAL, int ACT, bool WIDE = false>
+int launch_few(const bf16_t* x, const bf16_t* w0, const bf16_t* w1, int64_t M, int64_t N, int64_t K, bf16_t* out, void* gate, void* up,
+               hipStream_t stream) {
   const int tm = (int)((M + 15) / 16);
   // wavefronts: two pieces of the K range each where that is long enough for 16 of them
   int waves = 4;
@@ -706,7 +741,7 @@ int launch_few(const bf16_t* x, const bf16_t* w0, const bf16_t* w1, int64_t M, i
   const unsigned int lds = (unsigned)(waves * tm * (DUAL ? 2 : 1) * 64 * sizeof(f32x4));
   LaunchScope scope(MLC_KERNEL_FFN, stream, (DUAL ? 4.0 : 2.0) * M * N * K, 2.0 * ((DUAL ? 2.0 : 1.0) * N * K + (double)M * (N + K)));
 #define MLC_FEW(TM) \
-  hipLaunchKernelGGL((ffn_few_kernel<DUAL, ACT, TM>), grid, block, lds, stream, x, w0, w1, (int)M, (int)N, (int)K, out, gate, up)
+  hipLaunchKernelGGL((ffn_few_kernel<DUAL, ACT, TM, WIDE>), grid, block, lds, stream, x, w0, w1, (int)M, (int)N, (int)K, out, gate, up)
   if (tm == 1) MLC_FEW(1); else MLC_FEW(2);
 #undef MLC_FEW
   return check_launch();
@@ -714,11 +749,12 @@ int launch_few(const bf16_t* x, const bf16_t* w0, const bf16_t* w1, int64_t M, i
 
 template <int FORM, int ACT, int BM, int BN, int NB>
 int launch_tile(GemmArgs& g, const Plan& plan, double flops, double bytes, hipStream_t stream) {
+  constexpr int COLS = FORM == UP || FORM == UP32 ? BN / 2 : BN;
   long tiles = 0;
   for (int i = 0; i < g.problems; ++i) {
     Problem& p = g.p[i];
     p.tiles_m = (p.M + BM - 1) / BM;
-    p.tiles_n = (p.N + (FORM == UP ? BN / 2 : BN) - 1) / (FORM == UP ? BN / 2 : BN);
+    p.tiles_n = (p.N + COLS - 1) / COLS;
     p.first = (int)tiles;
     tiles += (long)p.tiles_m * p.tiles_n;
     if (tiles > (1L << 28)) return MLC_ERR_SHAPE;
@@ -753,9 +789,10 @@ int launch_form(GemmArgs& g, const Plan& plan, hipStream_t stream) {
   double flops = 0.0, bytes = 0.0;
   for (int i = 0; i < g.problems; ++i) {
     const Problem& p = g.p[i];
-    const double twice = FORM == UP || FORM == NN ? 2.0 : 1.0;
+    constexpr bool both = FORM == UP || FORM == UP32;
+    const double twice = both || FORM == NN ? 2.0 : 1.0;
     flops += 2.0 * twice * p.M * p.N * (double)p.K;
-    bytes += 2.0 * (twice * ((double)p.M * p.K / (FORM == UP ? 2 : 1) + (double)p.N * p.K) + (double)p.M * p.N);
+    bytes += 2.0 * (twice * ((double)p.M * p.K / (both ? 2 : 1) + (double)p.N * p.K) + (double)p.M * p.N);
   }
   if (plan.bm == 256) return launch_tile<FORM, ACT, 256, 256, 5>(g, plan, flops, bytes, stream);
   if (plan.bm == 128 && plan.per_unit == 1) return launch_tile<FORM, ACT, 128, 128, 9>(g, plan, flops, bytes, stream);
@@ -779,13 +816,16 @@ size_t ffn_backward_workspace(const FfnShape& s) {
   return 2 * (size_t)round_up(s.t * s.f * 2, 256) + (dx > dw ? dx : dw);
 }
 
-int launch_ffn_forward(const FfnShape& s, const bf16_t* x, const bf16_t* wg, const bf16_t* wu, const bf16_t* wd, bf16_t* gate, bf16_t* up,
+int launch_ffn_forward(const FfnShape& s, const bf16_t* x, const bf16_t* wg, const bf16_t* wu, const bf16_t* wd, void* gate, void* up,
                        bf16_t* hidden, bf16_t* y, void* workspace, hipStream_t stream) {
   int rc;
   const bool silu = s.act == MLC_ACT_SILU;
   if (few(s.t, s.f, s.d)) {
-    rc = silu ? launch_few<true, MLC_ACT_SILU>(x, wg, wu, s.t, s.f, s.d, hidden, gate, up, stream)
-              : launch_few<true, MLC_ACT_GELU_TANH>(x, wg, wu, s.t, s.f, s.d, hidden, gate, up, stream);
+    auto launch = [&](auto act, auto wide) {
+      return launch_few<true, decltype(act)::value, decltype(wide)::value>(x, wg, wu, s.t, s.f, s.d, hidden, gate, up, stream);
+    };
+    if (s.wide && gate) rc = silu ? launch(I<MLC_ACT_SILU>{}, std::true_type{}) : launch(I<MLC_ACT_GELU_TANH>{}, std::true_type{});
+    else rc = silu ? launch(I<MLC_ACT_SILU>{}, std::false_type{}) : launch(I<MLC_ACT_GELU_TANH>{}, std::false_type{});
   } else {
     GemmArgs g{};
     g.problems = 1;
@@ -793,7 +833,8 @@ int launch_ffn_forward(const FfnShape& s, const bf16_t* x, const bf16_t* wg, con
     g.p[0].B[1] = wu;
     g.gate = gate; g.up = up;
     const Plan both = plan_up(s.t, s.d, s.f);
-    rc = silu ? launch_form<UP, MLC_ACT_SILU>(g, both, stream) : launch_form<UP, MLC_ACT_GELU_TANH>(g, both, stream);
+    if (s.wide && gate) rc = silu ? launch_form<UP32, MLC_ACT_SILU>(g, both, stream) : launch_form<UP32, MLC_ACT_GELU_TANH>(g, both, stream);
+    else rc = silu ? launch_form<UP, MLC_ACT_SILU>(g, both, stream) : launch_form<UP, MLC_ACT_GELU_TANH>(g, both, stream);
   }
   if (rc != MLC_OK) return rc;
   if (few(s.t, s.d, s.f)) return launch_few<false, 0>(hidden, wd, wd, s.t, s.d, s.f, y, nullptr, nullptr, stream);
@@ -805,7 +846,7 @@ int launch_ffn_forward(const FfnShape& s, const bf16_t* x, const bf16_t* wg, con
 }
 
 int launch_ffn_backward(const FfnShape& s, const bf16_t* dy, const bf16_t* x, const bf16_t* wg, const bf16_t* wu, const bf16_t* wd,
-                        const bf16_t* gate, const bf16_t* up, const bf16_t* hidden, bf16_t* dx, bf16_t* dwg, bf16_t* dwu, bf16_t* dwd,
+                        const void* gate, const void* up, const bf16_t* hidden, bf16_t* dx, bf16_t* dwg, bf16_t* dwu, bf16_t* dwd,
                         void* workspace, hipStream_t stream) {
   bf16_t* const dg = (bf16_t*)workspace;
   bf16_t* const du = (bf16_t*)((unsigned char*)workspace + round_up(s.t * s.f * 2, 256));
@@ -814,10 +855,10 @@ int launch_ffn_backward(const FfnShape& s, const bf16_t* dy, const bf16_t* x, co
   if (s.t) {
     GemmArgs g{};
     g.problems = 1;
-      g.p[0] = problem(dy, s.d, wd, s.f, dg, s.f, s.t, s.f, s.d);
-    g.gate = const_cast<bf16_t*>(gate); g.up = const_cast<bf16_t*>(up); g.du = du;
+    g.p[0] = problem(dy, s.d, wd, s.f, dg, s.f, s.t, s.f, s.d);
+    g.gate = const_cast<void*>(gate); g.up = const_cast<void*>(up); g.du = du;
     const Plan inner = plan_inner(s.t, s.d, s.f);
-    rc = launch_form<DH>(g, inner, stream);
+    rc = s.wide ? launch_form<DH32>(g, inner, stream) : launch_form<DH>(g, inner, stream);
     if (rc != MLC_OK) return rc;
     GemmArgs n{};
     n.problems = 1;

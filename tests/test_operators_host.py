@@ -182,3 +182,12 @@ def test_heads_of_an_output_may_not_overlap(tokens, heads, token_stride, head_st
     first, second = ("dq", "dk") if back else ("q_out", "k_out")
     got = _qk(back, change=dict(tokens=tokens, q_heads=heads), heads={first: [P, token_stride, head_stride], second: None})
     assert got == (NULL if fine else ARG)
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_type_of_the_factors(back):
+    lib, ws = mlc.library(), [P, 1 << 30, None]
+    for flag, x, want in ((2, P, ARG), (-1, P, ARG), (1, None, NULL), (0, None, NULL)):
+        desc = B._GatedFFN(4, 64, 72, 0, x, P, P, P, flag)
+        got = lib.muloco_gated_ffn_backward(C.byref(desc), *[P] * 8, *ws) if back else lib.muloco_gated_ffn(C.byref(desc), *[P] * 4, *ws)
+        assert got == want, (flag, x)
