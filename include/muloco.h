@@ -5,10 +5,17 @@
  *   newton_schulz       quintic Newton-Schulz orthogonalisation of a batch of matrices
  *   muloco_inner_step   one Muon step (momentum, look-ahead, orthogonalisation, update)
  *   muloco_outer_step   one DiLoCo outer step over K resident worker replicas
- * plus muloco_quantize_delta, the compressor of the outer step as a call of its own.
+ * plus muloco_quantize_delta, the compressor of the outer step as a call of its own,
+ * muloco_topk_outer_step, the outer step with the other compressor, and what a training step
+ * needs beside them:
+ *   muloco_adamw_step, muloco_adamw8_step   AdamW for the parameters that are no hidden matrices,
+ *                       with states in 32 or in 8 bits (muloco_adamw8_values reads those out)
+ *   muloco_qk_norm_rope, muloco_gated_ffn   norm of q and k heads with rotary positions, and the
+ *                       gated feed-forward block, each with a _backward call
  *
  * Conventions shared by every call
- *   - Every data pointer is a DEVICE pointer owned by the caller and 16-byte aligned.
+ *   - Every data pointer is a DEVICE pointer owned by the caller and 16-byte aligned, unless
+ *     a call states less.
  *     Arrays of structs and arrays of pointers (groups, worker lists) are HOST memory and
  *     are only read during the call.
  *   - A "group" is `count` row-major matrices of one shape, contiguous: [count][m][n].
@@ -352,7 +359,8 @@ int muloco_adamw8_values(const mlc_adamw8_group* groups, int n_groups, float* co
  *     y = n with its first rot_dim values turned pairwise:
  *         y_a = n_a cos[p][i] - n_b sin[p][i] ; y_b = n_b cos[p][i] + n_a sin[p][i],  i < rot_dim / 2
  *     pairs (a, b) = (i, i + rot_dim / 2), or (2 i, 2 i + 1) with `interleaved`
- * in fp32, rounded once to `dtype`.  A position outside [0, table_rows) reads nothing and gives NaN.
+ * in fp32 (a head whose squares exceed its range becomes 0), rounded once to `dtype`.  A position outside [0, table_rows) reads
+ * nothing and gives NaN; with rot_dim 0 there are no positions.
  * The backward call takes the gradients of the outputs and the inputs of the forward call and gives the
  * gradients of q and k and, summed over tokens and heads in fp32 in an order that depends on the shapes alone,
  * of the gains.

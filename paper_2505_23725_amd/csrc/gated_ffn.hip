@@ -20,6 +20,9 @@
 // the matrix cores wait for it: with the activation's slope in it (20 instructions an element, two of them quarter rate)
 // a tile of 256 x 256 took 24 us beside its 46 us of products.
 //
+// 16384 x 2048 x 5632 (tiles of 256): UP 575 us, 1.32 PFLOP/s; NT 280, 1.35; DH 402, 0.94; NN 522, 1.45; TN 789, 1.44: the matrix cores at
+// the power limit, but for the epilogues of UP and DH.
+//
 // Tiles: 256 threads, 2 x 2 wavefronts, operands straight from memory to LDS in a ring of 64-deep K tiles, the fragments of one
 // 32-deep slice read while the matrix cores work on the one before it: the scheme of the Newton-Schulz products
 // (ns_gemm.hip), with nothing padded: what lies outside a matrix is beyond the end of its buffer resource, whose loads give

@@ -10,7 +10,9 @@
 //
 // Bound by the memory stream: a row is read once and written once (backwards two rows in, one out).  L lanes share a row, a lane
 // holds four pairs, and a group of L lanes takes HEADS heads of one token after the other, so that a row of the tables is read
-// once for them, their loads are all under way together and the gains stay in registers.
+// once for them, their loads are all under way together and the gains stay in registers.  16384 tokens x 32 heads of 128 in bf16: forward
+// 62 us, 337 MB with the tables for every four heads, 5.4 TB/s; backward 83, 471 MB, 5.7 TB/s, and 5 for the gains' sums.  Where head or
+// rotated width is no multiple of 8, elements go one by one: half that rate (100 / 100: forward 99 us, 210 MB).
 //
 // The gains' gradients are sums over all tokens and heads: a lane keeps its own elements' sums in registers over all rows it
 // meets, a workgroup adds its lanes' and writes one partial row, and a second kernel adds the partial rows, each

@@ -76,3 +76,13 @@ def test_forward_and_backward(dim, rot, inter, dtype, tokens, hq, hk, offset):
         _rows_close(y[i], ry, what)
         _rows_close(dx[i], rx, "d" + what)
         assert (dw[i].double() - rw).norm() <= EW_TOL * rw.norm(), what
+
+
+def test_squares_beyond_the_range():
+    """(as the header states it; the largest whose squares still fit are normed as any others)"""
+    x = torch.full((2, 2, 64), 1e18, device=DEV)
+    x[1] = 1e30
+    one, none, pos = torch.ones(64, device=DEV), torch.empty(0, 0, device=DEV), torch.zeros(2, dtype=torch.int64, device=DEV)
+    y, k = torch.empty_like(x), torch.empty(2, 0, 64, device=DEV)
+    mlc.muloco_qk_norm_rope(x, k, one, one, none, none, pos, y, k)
+    assert torch.allclose(y[0], torch.ones_like(y[0]), rtol=1e-6) and not y[1].any()
